@@ -181,8 +181,12 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
 #pragma unroll
                 for (int n = 0; n < N; ++n) dhp[h][r][n] = dh.get(col + n < q2_count ? mixed_row(16 * h + 4 * g + r) * a.Q2 + col + n : NOWHERE);
     };
-    // Logits that are no word's: in columns past n2, and in the last column q1 of a vocabulary in some columns q2.  Chunks that hold some mask them.
-    const bool edge = OP == OP_LOSS && q2_count < Sh::R2;
+    // Logits that are no word's: in columns past n2, and in the last column q1 of a vocabulary in some columns q2.  Wavefronts and chunks that
+    // hold some mask them, in the form that also takes the 1 off the target.
+    const bool edge = OP == OP_LOSS && (wave + 1) * 16 * N > q2_count;
+    int words[N];                          // columns q1 of the block, from the first, that are words in each of this lane's columns q2
+#pragma unroll
+    for (int n = 0; n < N; ++n) words[n] = col + n < q2_count ? a.Q1 - q1_first - (OP == OP_LOSS && (int64_t)(a.Q1 - 1) * a.Q2 + q2_first + col + n >= a.vocab) : 0;
     const int cut_chunk = OP == OP_LOSS && (int64_t)a.Q1 * a.Q2 > a.vocab && a.Q1 - q1_first <= q1_count ? nchunks - 1 : -1;
 
     int t = blockIdx.x;
@@ -229,21 +233,20 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
     while (t < a.tokens) {
         const T* const x = (const T*)a.x + t * a.ldx;
         // The loss: logits are in units of log 2, and their products' sums start from -lse, so exponentials of Z are the probabilities.
-        // The token's weight comes in with U for dF1 and with dU.  The target, whose
-        // dZ is less by one, is taken out of dF1 and dU where they are.
+        // The token's weight comes in with U for dF1 and with dU.  The target's dZ, p - 1, is taken before it is rounded, by the
+        // wavefront that has its column, in its chunk.
         float weight = 1.0f, from = 0.0f;
-        int target_q1 = -1, target_row = 0;                // in this block: column q1; row of U's fragments.  -1: it has no part in the target
-        f32x4 ut[Sh::EP];
+        int target_q1 = -1, target_q2 = -1;                // its place in the block; -1: not this wavefront's
         if constexpr (OP == OP_LOSS) {
             const int q1 = (int)((unsigned)target / (unsigned)a.Q2), q2 = (int)target - q1 * a.Q2 - q2_first;
-            if (q1 >= q1_first && q1 < q1_first + q1_count && q2 >= 0 && q2 < q2_count) {
-                target_q1 = q1 - q1_first;
-                const int in = q2 % (16 * N);
-                target_row = q2 - in + (in % N) * 16 + in / N;
-            }
+            const bool here = q1 >= q1_first && q1 < q1_first + q1_count && q2 >= 0 && q2 < q2_count && q2 / (16 * N) == wave;
+            target_q1 = __builtin_amdgcn_readfirstlane(here ? q1 - q1_first : -1);
+            target_q2 = __builtin_amdgcn_readfirstlane(here ? q2 : -1);
             weight = dloss;
             from = -lse * LOG2E;
         }
+        const int target_chunk = target_q1 >> 5;
+        static_assert(Sh::C1 == 32, "rows of a chunk");
         const f32x4 start = {from, from, from, from};
         store_x(x);
         __syncthreads();
@@ -293,7 +296,7 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
         }
 
         // A chunk's Z, dZ, what it adds to dU, and dZ into LDS.  No branches: what a wavefront has next to do beside it fills its waits.
-        auto z_part = [&](int ch, auto masked) __attribute__((always_inline)) {
+        auto z_part = [&](int ch, auto marked) __attribute__((always_inline)) {
             T* const szb = sz + (ch % Sh::DEEP) * BR * Sh::DZ;
             Piece d[OP == OP_LOSS ? 1 : BC][4];
             if constexpr (OP != OP_LOSS) {
@@ -340,14 +343,15 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
                                 z[1][n][r] = dv * act;
                             }
                         }
-                    if constexpr (masked.value) {
-                        const int row = q1_first + (ch * BC + pair * 2) * 16 + mixed_row(16 * h + 4 * g);
-                        const int64_t first = (int64_t)row * a.Q2 + q2_first + col;
+                    if constexpr (marked.value) {
+                        const int row = (ch * BC + pair * 2) * 16 + mixed_row(16 * h + 4 * g);
 #pragma unroll
-                        for (int n = 0; n < N; ++n)
+                        for (int n = 0; n < N; ++n) {
+                            int end = words[n], hit = target_q2 == col + n ? target_q1 : -1;
+                            asm volatile("" : "+v"(end), "+v"(hit));      // (or comparisons for all chunks would be kept in registers)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (col + n >= q2_count || first + (int64_t)r * a.Q2 + n >= a.vocab) z[0][n][r] = 0.0f;
+                            for (int r = 0; r < 4; ++r) z[0][n][r] = row + r < end ? z[0][n][r] - (row + r == hit ? 1.0f : 0.0f) : 0.0f;
+                        }
                     }
                 }
 #pragma unroll
@@ -407,20 +411,11 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
                     for (int d = 0; d < Sh::EP; ++d)
 #pragma unroll
                         for (int e = 0; e < Sh::EQ; ++e) df1[ch][b][d][e] += odd[d][e];
-                // minus the target's row of U (dU's share of it stands below)
-                if constexpr (OP == OP_LOSS)
-#pragma unroll
-                    for (int d = 0; d < Sh::EP; ++d)
-#pragma unroll
-                        for (int e = 0; e < Sh::EQ; ++e)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (target_q1 == (ch * BC + wq + e * Sh::WQ) * 16 + c) df1[ch][b][d][e][r] -= ut[d][r];
             }
         };
         auto z_of = [&](int ch) __attribute__((always_inline)) {
             if constexpr (OP == OP_LOSS) {
-                if (edge || ch == cut_chunk) z_part(ch, Yes());
+                if (edge || ch == cut_chunk || ch == target_chunk) z_part(ch, Yes());
                 else z_part(ch, No());
             } else z_part(ch, No());
         };
@@ -429,20 +424,13 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
         for (int ch = 0; ch < CHUNKS; ++ch) {
             if (ch >= nchunks) continue;
             __syncthreads();
-            if (ch == 0) {
-                if constexpr (Sh::UREG)
+            if (Sh::UREG && ch == 0)
 #pragma unroll
-                    for (int b = 0; b < BR; ++b)
-#pragma unroll
-                        for (int d = 0; d < Sh::EP; ++d)
-#pragma unroll
-                            for (int k = 0; k < KCQ; ++k) ur[b][d][k] = at.template crossed_columns<N>(su + b * Sh::UL, 2 * k, KC1, min(wp + d * Sh::WP, B1 - 1));
-                if constexpr (OP == OP_LOSS)
+                for (int b = 0; b < BR; ++b)
 #pragma unroll
                     for (int d = 0; d < Sh::EP; ++d)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) ut[d][r] = to_f32<T>(*frag_slot_at<MIXED>(su, target_row, 16 * min(wp + d * Sh::WP, B1 - 1) + 4 * g + r, KC1));
-            }
+                        for (int k = 0; k < KCQ; ++k) ur[b][d][k] = at.template crossed_columns<N>(su + b * Sh::UL, 2 * k, KC1, min(wp + d * Sh::WP, B1 - 1));
             f_part(ch);
             if (ch + 1 < CHUNKS && ch + 1 < nchunks) {
                 if constexpr (Sh::DEEP == 1) __syncthreads();             // dZ's buffer is free again
@@ -450,17 +438,6 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
             }
         }
         __syncthreads();                   // so is U
-
-        // the target's share of dU: minus its column of F1
-        if constexpr (OP == OP_LOSS)
-            if (target_q1 >= 0 && target_row / (16 * N) == wave)
-#pragma unroll
-                for (int n = 0; n < N; ++n)
-                    if (target_row % (16 * N) == n * 16 + c)
-#pragma unroll
-                        for (int i = 0; i < B1; ++i)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) du[0][i][n][r] -= to_f32<T>(*frag_slot_at<MIXED>(s1, mixed_row(target_q1), 16 * i + 4 * g + r, KC1));
 
         // dF2 from dU in registers; dU through LDS, in U's place, for dX
         Frag df[BR][KC1][N];
