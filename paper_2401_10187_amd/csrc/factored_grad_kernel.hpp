@@ -181,13 +181,13 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
 #pragma unroll
                 for (int n = 0; n < N; ++n) dhp[h][r][n] = dh.get(col + n < q2_count ? mixed_row(16 * h + 4 * g + r) * a.Q2 + col + n : NOWHERE);
     };
-    // Logits that are no word's: in columns past n2, and in the last column q1 of a vocabulary in some columns q2.  Wavefronts and chunks that
-    // hold some mask them, in the form that also takes the 1 off the target.
+    // Logits that are no word's: in columns past n2, in rows past Q1, and in the last column q1 of a vocabulary in some columns q2.  Wavefronts and
+    // chunks that hold some mask them, in the form that also takes the 1 off the target.  (F1's zeros there do not: Z is -lse, whose exponential may be infinite.)
     const bool edge = OP == OP_LOSS && (wave + 1) * 16 * N > q2_count;
     int words[N];                          // columns q1 of the block, from the first, that are words in each of this lane's columns q2
 #pragma unroll
     for (int n = 0; n < N; ++n) words[n] = col + n < q2_count ? a.Q1 - q1_first - (OP == OP_LOSS && (int64_t)(a.Q1 - 1) * a.Q2 + q2_first + col + n >= a.vocab) : 0;
-    const int cut_chunk = OP == OP_LOSS && (int64_t)a.Q1 * a.Q2 > a.vocab && a.Q1 - q1_first <= q1_count ? nchunks - 1 : -1;
+    const int cut_chunk = OP == OP_LOSS && ((int64_t)a.Q1 * a.Q2 > a.vocab || a.Q1 % Sh::C1) && a.Q1 - q1_first <= q1_count ? nchunks - 1 : -1;
 
     int t = blockIdx.x;
     // A token's target, weight and logarithm of the sum; the next token's are loaded while one is worked on
