@@ -291,12 +291,13 @@ template <typename T> struct Span {
 // read unaligned, 16 bytes at once).  A fragment's places outside P1 x P2 get some other elements of the same row: their
 // factor's row is zeros, and what an infinity or NaN there spoils is the token's own results, all of which it is part of anyhow.  So
 // there is no choice between loaded values and zeros that would have to wait for them.  `near_end`: some lane may need fewer than eight; it reads the
-// row's last eight and moves them down.  `first`: the fragment is the one in front, the only one of rows of fewer than eight.
-template <typename T> __device__ __forceinline__ typename Op<T>::Frag eight_of_row(const T* __restrict__ x, int at, bool inside, int total, bool near_end, bool first)
+// row's last eight and moves them down.  WHOLE: no row has fewer than eight elements, as in all classes of factors but the first.  Shorter ones are read
+// one by one; `first`: some of a short row may be in this fragment.
+template <bool WHOLE, typename T> __device__ __forceinline__ typename Op<T>::Frag eight_of_row(const T* __restrict__ x, int at, bool inside, int total, bool near_end, bool first)
 {
     typedef typename Op<T>::Frag Frag;
     Frag f = {};
-    if (total >= 8) {
+    if (WHOLE || total >= 8) {
         at = inside ? at : 0;
         const int from = min(at, total - 8);
         __builtin_memcpy(&f, x + from, sizeof f);

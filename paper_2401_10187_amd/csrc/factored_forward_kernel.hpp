@@ -77,7 +77,9 @@ __global__ __launch_bounds__(THREADS) void factored_forward(ForwardArgs a)
 #pragma unroll
         for (int i = 0; i < B1; ++i) {
             const int p1 = mixed_row(16 * i + c), p2 = 32 * k + 8 * g;
-            f[i] = eight_of_row(x, p1 * a.P2 + p2, p1 < a.P1 && p2 < a.P2, total, ragged && (16 * (i | 1) + 15) * a.P2 + 32 * k + 32 > total, i == 0 && k == 0);
+            // Short rows are in two fragments: p1 = 4 to 6 are in the second one.  (Classes without them ask for them all the same, and then read nothing: the
+            // loads are scheduled better so.  1500 tokens 128x128,128x256: 62.5 us, 65.2 with WHOLE; one token 64x128,64x128 5.4, 5.8.)
+            f[i] = eight_of_row<false>(x, p1 * a.P2 + p2, p1 < a.P1 && p2 < a.P2, total, ragged && (16 * (i | 1) + 15) * a.P2 + 32 * k + 32 > total, KC1 * KC2 == 1);
         }
     };
     if constexpr (AHEAD)

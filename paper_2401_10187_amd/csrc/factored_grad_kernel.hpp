@@ -158,14 +158,14 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
 #pragma unroll
         for (int i = 0; i < Sh::XAHEAD; ++i) {
             const int piece = tid + i * THREADS, p1 = piece * magic >> 16, k = 8 * (piece - p1 * row_pieces);
-            xp[i] = eight_of_row(x, p1 * a.P2 + k, piece < pieces, total, a.P2 % 8 != 0, i == 0);
+            xp[i] = eight_of_row<(KC1 * KC2 > 1)>(x, p1 * a.P2 + k, piece < pieces, total, a.P2 % 8 != 0, i == 0);
         }
     };
     auto store_x = [&](const T* x) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < Sh::XPIECES; ++i) {
             const int piece = tid + i * THREADS, p1 = piece * magic >> 16, k = 8 * (piece - p1 * row_pieces);
-            if (piece < pieces) at.put_straight(sx, mixed_row(p1), k, KC2, i < Sh::XAHEAD ? xp[i] : eight_of_row(x, p1 * a.P2 + k, true, total, a.P2 % 8 != 0, false));
+            if (piece < pieces) at.put_straight(sx, mixed_row(p1), k, KC2, i < Sh::XAHEAD ? xp[i] : eight_of_row<(KC1 * KC2 > 1)>(x, p1 * a.P2 + k, true, total, a.P2 % 8 != 0, false));
         }
     };
 
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
 #pragma unroll
                 for (int i = 0; i < B1; ++i) {
                     const Frag xf = Sh::XLDS ? at.get(sx, i * KC2 + k)
-                                             : eight_of_row(x, mixed_row(16 * i + c) * a.P2 + 32 * k + 8 * g, mixed_row(16 * i + c) < a.P1 && 32 * k + 8 * g < a.P2, total, a.P2 % 8 != 0, i == 0 && k == 0);
+                                             : eight_of_row<(KC1 * KC2 > 1)>(x, mixed_row(16 * i + c) * a.P2 + 32 * k + 8 * g, mixed_row(16 * i + c) < a.P1 && 32 * k + 8 * g < a.P2, total, a.P2 % 8 != 0, true);
 #pragma unroll
                     for (int n = 0; n < N; ++n) Op<T>::mma(du[b][i][n], xf, f[n]);
                 }
