@@ -331,13 +331,14 @@ template <bool GELU> __device__ __forceinline__ float activate(float z, float& s
     return z * s;
 }
 
-// act(z) * u for the forward pass, where SiLU's z comes times log2 e, which the divisor takes back.
+// act(z) * u for the forward pass, where SiLU's z comes times log2 e, which the divisor takes back.  u comes last: z * u may be infinite where a closed
+// gate makes the result 0.
 template <bool GELU> __device__ __forceinline__ float gate(float z, float u)
 {
     if constexpr (GELU) {
         float slope;
         return activate<true>(z, slope) * u;
-    } else return z * u * __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_amdgcn_exp2f(-z), LOG2E, LOG2E));
+    } else return z * __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_amdgcn_exp2f(-z), LOG2E, LOG2E)) * u;
 }
 
 struct Yes { static constexpr bool value = true; };

@@ -339,7 +339,7 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
                             else {
                                 float slope;
                                 const float act = activate<OP == OP_GELU>(z[0][n][r], slope), dv = to_f32<T>(d[pair * 2 + h][r][n]);
-                                z[0][n][r] = dv * z[1][n][r] * slope;
+                                z[0][n][r] = slope * z[1][n][r] * dv;      // (a slope of 0 first: the others' product may be infinite)
                                 z[1][n][r] = dv * act;
                             }
                         }
