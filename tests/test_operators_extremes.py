@@ -26,3 +26,20 @@ def test_a_closed_gate_closes(act, dtype, t):
     dh[:, 2] = 0
     for got in (lambda a, b, c: (a, *b, *c))(*km.kron_gated_grad(dh, x, gate, up, act=act)):
         assert not got.any()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+def test_slopes_of_wide_open_and_closed_gates(act, dtype):
+    """z = 1e20, whose square is no number in single precision: slope 1; z = -1e20: slope 0.  Values are right to one rounding of the type, or in single
+    precision to four."""
+    one = torch.ones((1, 1), device="cuda", dtype=dtype)
+    x, dh = torch.ones((1, 1), device="cuda", dtype=dtype), torch.ones((1, 4), device="cuda", dtype=dtype)
+    gate, up = (column(dtype, 1e20, -1e20, 1e38, -1e38), one), (column(dtype, 1.0, 1.0, 1.0, 1.0), one)
+    bound = 2 ** -22 if dtype == torch.float32 else 2 ** -8
+    want = gate[0].double().clamp(min=0)
+    assert bool(((km.kron_gated(x, gate, up, act=act).double() - want).abs() <= bound * want).all())
+    dh[0, 2:] = 0            # (their sum with the others' is no number)
+    _, (dg, _), (du, _) = km.kron_gated_grad(dh, x, gate, up, act=act)
+    assert dg.float().tolist() == [[1.0, 0.0, 0.0, 0.0]]
+    assert bool(((du.double() - dh.double() * want).abs() <= bound * want).all())
