@@ -149,6 +149,10 @@ km_status check_shape(int M, const int* P, const int* Q, km_dtype dtype, Shape& 
 
 // The part of the product that a vocabulary reaches into.
 struct Columns { int q1, q2; };
+// Columns q1 beyond these need more than a launch's 65535 blocks in every variant (the widest block is 160 KB of LDS, 64 bytes a column), and less than a
+// block more of them is within 32 bits, so that plans can be made of any number up to here.
+constexpr int MOST_Q1 = 1 << 28;
+km_status check_columns(km_status shape, Columns cols) { return shape == KM_OK && cols.q1 > MOST_Q1 ? KM_EUNSUPPORTED : shape; }
 Columns columns_of(const Shape& s, int64_t vocab)
 {
     return {(int)((vocab + s.Q2 - 1) / s.Q2), (int)(vocab < s.Q2 ? vocab : s.Q2)};
@@ -388,9 +392,11 @@ km_status kronmatmul_gated(int M, const int* P, const int* Q, const void* X, lon
                            void* H, km_dtype dtype, void* stream)
 {
     Shape s;
-    const km_status ok = check_shape(M, P, Q, dtype, s);
+    km_status ok = check_shape(M, P, Q, dtype, s);
     if (ok != KM_OK && ok != KM_EUNSUPPORTED) return ok;
     if (act != KM_ACT_SILU && act != KM_ACT_GELU_TANH) return KM_EINVAL;
+    const Columns cols = {Q[0], Q[1]};
+    ok = check_columns(ok, cols);
     if (!X || !H || !gate || !up_ || ldx < (int64_t)P[0] * P[1]) return KM_EINVAL;
     const size_t size = element_size(dtype);
     Region in[5] = {{X, reach(M, ldx, (int64_t)P[0] * P[1], size)}};
@@ -403,7 +409,6 @@ km_status kronmatmul_gated(int M, const int* P, const int* Q, const void* X, lon
     if (!fits(X, size) || !fits(H, size) || collide(out, 1, in, 5)) return KM_EINVAL;
     if (ok != KM_OK || M == 0) return ok;
     const int op = act == KM_ACT_SILU ? OP_SILU : OP_GELU;
-    const Columns cols = {s.Q1, s.Q2};
     ForwardArgs a = {};
     a.x = X; a.y = H; a.ldx = ldx;
     a.f1[0] = gate[0]; a.f2[0] = gate[1]; a.f1[1] = up_[0]; a.f2[1] = up_[1];
@@ -414,9 +419,12 @@ km_status kronmatmul_gated_grad_workspace_size(int M, const int* P, const int* Q
 {
     Shape s;
     if (!bytes) return KM_EINVAL;
-    const km_status ok = check_shape(M, P, Q, dtype, s);
+    km_status ok = check_shape(M, P, Q, dtype, s);
     if (ok != KM_OK) return ok;
-    *bytes = plan_grad(OP_SILU, dtype, M, s, {s.Q1, s.Q2}).bytes;      // (both activations have the same variants)
+    const Columns cols = {s.Q1, s.Q2};
+    ok = check_columns(ok, cols);
+    if (ok != KM_OK) return ok;
+    *bytes = plan_grad(OP_SILU, dtype, M, s, cols).bytes;      // (both activations have the same variants)
     return KM_OK;
 }
 
@@ -425,9 +433,11 @@ km_status kronmatmul_gated_grad(int M, const int* P, const int* Q, const void* d
                                 size_t workspace_bytes, void* stream)
 {
     Shape s;
-    const km_status ok = check_shape(M, P, Q, dtype, s);
+    km_status ok = check_shape(M, P, Q, dtype, s);
     if (ok != KM_OK && ok != KM_EUNSUPPORTED) return ok;
     if (act != KM_ACT_SILU && act != KM_ACT_GELU_TANH) return KM_EINVAL;
+    const Columns cols = {Q[0], Q[1]};
+    ok = check_columns(ok, cols);
     if (!X || !dH || !dX || !gate || !up_ || !dgate || !dup || ldx < (int64_t)P[0] * P[1] || lddh < (int64_t)Q[0] * Q[1]) return KM_EINVAL;
     const size_t size = element_size(dtype);
     Region in[6] = {{X, reach(M, ldx, (int64_t)P[0] * P[1], size)}, {dH, reach(M, lddh, (int64_t)Q[0] * Q[1], size)}};
@@ -444,7 +454,6 @@ km_status kronmatmul_gated_grad(int M, const int* P, const int* Q, const void* d
     }
     if (!fits(X, size) || !fits(dH, size) || !fits(dX, size)) return KM_EINVAL;
     const int op = act == KM_ACT_SILU ? OP_SILU : OP_GELU;
-    const Columns cols = {Q[0], Q[1]};
     out[5] = {workspace, ok == KM_OK ? plan_grad(op, dtype, M, s, cols).bytes : 0};
     if (collide(out, 6, in, 6)) return KM_EINVAL;
     if (ok != KM_OK) return ok;
@@ -458,10 +467,13 @@ km_status kronmatmul_cross_entropy_workspace_size(int M, const int* P, const int
 {
     Shape s;
     if (!bytes) return KM_EINVAL;
-    const km_status ok = check_shape(M, P, Q, dtype, s);
+    km_status ok = check_shape(M, P, Q, dtype, s);
     if (ok != KM_OK) return ok;
     if (vocab < 1 || vocab > (int64_t)s.Q1 * s.Q2) return KM_EINVAL;
-    *bytes = M ? piece((size_t)M * plan_forward(OP_LOSS, dtype, M, s, columns_of(s, vocab)).parts * 8) + (size_t)M * 4 : 0;
+    const Columns cols = columns_of(s, vocab);
+    ok = check_columns(ok, cols);
+    if (ok != KM_OK) return ok;
+    *bytes = M ? piece((size_t)M * plan_forward(OP_LOSS, dtype, M, s, cols).parts * 8) + (size_t)M * 4 : 0;
     return KM_OK;
 }
 
@@ -469,13 +481,14 @@ km_status kronmatmul_cross_entropy(int M, const int* P, const int* Q, long long 
                                    const long long* targets, float* loss, float* lse, km_dtype dtype, void* workspace, size_t workspace_bytes, void* stream)
 {
     Shape s;
-    const km_status ok = check_shape(M, P, Q, dtype, s);
+    km_status ok = check_shape(M, P, Q, dtype, s);
     if (ok != KM_OK && ok != KM_EUNSUPPORTED) return ok;
     if (!X || !F || !F[0] || !F[1] || !targets || !loss || !lse || ldx < (int64_t)P[0] * P[1]) return KM_EINVAL;
     if (vocab < 1 || vocab > (int64_t)Q[0] * Q[1]) return KM_EINVAL;
     const size_t size = element_size(dtype);
     if (!fits(X, size) || !fits(F[0], size) || !fits(F[1], size) || !fits(targets, 8) || !fits(loss, 4) || !fits(lse, 4)) return KM_EINVAL;
     const Columns cols = columns_of({P[0], Q[0], P[1], Q[1]}, vocab);
+    ok = check_columns(ok, cols);
     ForwardPlan p = {};
     size_t first = 0, need = 0;
     if (ok == KM_OK && M) {
@@ -505,10 +518,13 @@ km_status kronmatmul_cross_entropy_grad_workspace_size(int M, const int* P, cons
 {
     Shape s;
     if (!bytes) return KM_EINVAL;
-    const km_status ok = check_shape(M, P, Q, dtype, s);
+    km_status ok = check_shape(M, P, Q, dtype, s);
     if (ok != KM_OK) return ok;
     if (vocab < 1 || vocab > (int64_t)s.Q1 * s.Q2) return KM_EINVAL;
-    *bytes = plan_grad(OP_LOSS, dtype, M, s, columns_of(s, vocab)).bytes;
+    const Columns cols = columns_of(s, vocab);
+    ok = check_columns(ok, cols);
+    if (ok != KM_OK) return ok;
+    *bytes = plan_grad(OP_LOSS, dtype, M, s, cols).bytes;
     return KM_OK;
 }
 
@@ -517,7 +533,7 @@ km_status kronmatmul_cross_entropy_grad(int M, const int* P, const int* Q, long 
                                         void* workspace, size_t workspace_bytes, void* stream)
 {
     Shape s;
-    const km_status ok = check_shape(M, P, Q, dtype, s);
+    km_status ok = check_shape(M, P, Q, dtype, s);
     if (ok != KM_OK && ok != KM_EUNSUPPORTED) return ok;
     if (!X || !F || !F[0] || !F[1] || !targets || !dloss || !lse || !dX || !dF || !dF[0] || !dF[1] || ldx < (int64_t)P[0] * P[1]) return KM_EINVAL;
     if (vocab < 1 || vocab > (int64_t)Q[0] * Q[1]) return KM_EINVAL;
@@ -526,6 +542,7 @@ km_status kronmatmul_cross_entropy_grad(int M, const int* P, const int* Q, long 
         !fits(dloss, 4) || !fits(lse, 4))
         return KM_EINVAL;
     const Columns cols = columns_of({P[0], Q[0], P[1], Q[1]}, vocab);
+    ok = check_columns(ok, cols);
     const size_t b1 = (size_t)P[0] * Q[0] * size, b2 = (size_t)P[1] * Q[1] * size;
     const Region in[] = {{X, reach(M, ldx, (int64_t)P[0] * P[1], size)}, {F[0], b1}, {F[1], b2}, {targets, (size_t)M * 8}, {dloss, (size_t)M * 4}, {lse, (size_t)M * 4}};
     const Region out[] = {{dX, (size_t)M * P[0] * P[1] * size}, {dF[0], b1}, {dF[1], b2}, {workspace, ok == KM_OK ? plan_grad(OP_LOSS, dtype, M, s, cols).bytes : 0}};
