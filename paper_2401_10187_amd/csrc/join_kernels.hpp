@@ -17,14 +17,17 @@ struct SumJob {
     int64_t blocks;                        // workgroups before the next job's (set by sum_up)
 };
 constexpr int SUM_FEW = 16, SUM_JOBS = 5;
-struct SumArgs { SumJob job[SUM_JOBS]; };
+struct SumArgs {
+    SumJob job[SUM_JOBS];
+    int64_t first;                         // of all workgroups, where this launch's start (set by sum_up)
+};
 
 inline int sum_span(const SumJob& j) { return j.parts <= SUM_FEW ? 1024 : 64; }
 
 template <typename T>
 __global__ __launch_bounds__(256) void sum_parts(SumArgs a)
 {
-    int64_t block = blockIdx.x;
+    int64_t block = a.first + blockIdx.x;
     int which = 0;
     while (which + 1 < SUM_JOBS && block >= a.job[which].blocks) block -= a.job[which++].blocks;
     const SumJob job = a.job[which];

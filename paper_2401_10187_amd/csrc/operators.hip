@@ -24,6 +24,9 @@ constexpr int MOST_COLUMNS = 1 << 22;      // and reach 64 rows of Q2 elements i
 // Blocks of columns are a launch's y and z.
 bool launchable(dim3 grid) { return grid.y <= 65535 && grid.z <= 65535; }
 
+// HIP takes fewer than 2^32 work-items along a launch (workgroups have up to 1024): what has more workgroups than these is several launches.
+constexpr int MOST_GROUPS = 1 << 21;
+
 // Workgroups that are worth having: one on each compute unit.
 constexpr int UNITS = 256;
 
@@ -72,11 +75,14 @@ hipError_t sum_up(SumArgs& a, int jobs, km_dtype dtype, hipStream_t stream)
         a.job[i].blocks = (a.job[i].n + sum_span(a.job[i]) - 1) / sum_span(a.job[i]);
         blocks += a.job[i].blocks;
     }
-    if (blocks == 0) return hipSuccess;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    if (dtype == KM_F32) hipLaunchKernelGGL(sum_parts<float>, dim3((unsigned)blocks), dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL(sum_parts<bf16>, dim3((unsigned)blocks), dim3(256), 0, stream, a);
-    return hipGetLastError();
+    for (a.first = 0; a.first < blocks; a.first += MOST_GROUPS) {
+        const unsigned groups = (unsigned)(blocks - a.first < MOST_GROUPS ? blocks - a.first : MOST_GROUPS);
+        if (dtype == KM_F32) hipLaunchKernelGGL(sum_parts<float>, dim3(groups), dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL(sum_parts<bf16>, dim3(groups), dim3(256), 0, stream, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // ---- layer norm
@@ -98,7 +104,20 @@ Team team_for(int H, int vec, bool backward)
 
 template <typename T, int VEC> hipError_t norm_forward_of(const NormArgs& a, Team team, hipStream_t stream)
 {
-    const int teams = team.threads < 256 ? 256 / team.threads : 1;
+    const int teams = team.threads < 256 ? 256 / team.threads : 1, most = teams * MOST_GROUPS, rows = a.rows;
+    if (rows > most) {
+        for (int first = 0; first < rows; first += most) {
+            NormArgs some = a;
+            some.x = (const T*)a.x + first * a.ldx;
+            some.y = (T*)a.y + (int64_t)first * a.H;
+            some.mean += first;
+            some.rstd += first;
+            some.rows = rows - first < most ? rows - first : most;
+            const hipError_t e = norm_forward_of<T, VEC>(some, team, stream);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
     const dim3 grid((a.rows + teams - 1) / teams);
     if (team.pieces == 0) hipLaunchKernelGGL((norm_forward<T, VEC, 256, 0>), grid, dim3(256), 0, stream, a);
     else if (team.threads == 64) hipLaunchKernelGGL((norm_forward<T, VEC, 64, 2>), grid, dim3(256), 0, stream, a);
@@ -510,8 +529,14 @@ km_status kronmatmul_cross_entropy(int M, const int* P, const int* Q, long long 
     a.picked = (float*)((char*)workspace + first);
     const km_status ran = run_forward(OP_LOSS, dtype, p, a, M, s, cols, (hipStream_t)stream);
     if (ran != KM_OK) return ran;
-    hipLaunchKernelGGL(loss_join, dim3((M + 15) / 16), dim3(256), 0, (hipStream_t)stream, a.partial, a.picked, a.targets, (int64_t)vocab, M, p.parts, loss, lse);
-    return done(hipGetLastError());
+    for (int first = 0; first < M; first += 16 * MOST_GROUPS) {
+        const int tokens = M - first < 16 * MOST_GROUPS ? M - first : 16 * MOST_GROUPS;
+        hipLaunchKernelGGL(loss_join, dim3((tokens + 15) / 16), dim3(256), 0, (hipStream_t)stream, a.partial + (int64_t)first * p.parts, a.picked + first, a.targets + first,
+                           (int64_t)vocab, tokens, p.parts, loss + first, lse + first);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return done(e);
+    }
+    return KM_OK;
 }
 
 km_status kronmatmul_cross_entropy_grad_workspace_size(int M, const int* P, const int* Q, long long vocab, km_dtype dtype, size_t* bytes)

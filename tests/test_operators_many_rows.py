@@ -1,0 +1,76 @@
+"""Rows, tokens and columns beyond one launch: HIP takes fewer than 2^32 work-items.  Every row is one of 64, whose results are known from a small call."""
+import pytest
+
+torch = pytest.importorskip("torch")
+import paper_2401_10187_amd as km  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def enough(gib):
+    free = torch.cuda.mem_get_info()[0]
+    if free < gib << 30:
+        pytest.skip("needs %d GiB of device memory, %d are free" % (gib, free >> 30))
+
+
+def repeated(base, rows):
+    """`rows` rows, row i being row i % 64 of `base`."""
+    out = torch.empty((rows, *base.shape[1:]), dtype=base.dtype, device="cuda")
+    whole = rows // 64 * 64
+    out[:whole].view(-1, *base.shape).copy_(base.expand(whole // 64, *base.shape))
+    out[whole:] = base[:rows - whole]
+    return out
+
+
+def repeats(got, base):
+    whole = len(got) // 64 * 64
+    return bool((got[:whole].view(-1, *base.shape) == base).all()) and torch.equal(got[whole:], base[:len(got) - whole])
+
+
+# four rows to a workgroup of 256; one
+@pytest.mark.parametrize("rows,width", [((1 << 26) + 5, 8), ((1 << 24) + 3, 129)])
+def test_layer_norm(rows, width):
+    enough(40)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    base = torch.randn((64, width), generator=g, device="cuda").bfloat16()
+    w, b = torch.randn((2, width), generator=g, device="cuda").bfloat16().unbind()
+    w, b = w.clone(), b.clone()
+    want = km.layer_norm(base, w, b)
+    x = repeated(base, rows)
+    got = km.layer_norm(x, w, b)
+    assert all(repeats(p, q) for p, q in zip(got, want))
+    dwant = km.layer_norm_grad(base, base, w, *want[1:])[0]
+    assert repeats(km.layer_norm_grad(x, x, w, *got[1:])[0], dwant)
+
+
+def test_loss():
+    enough(40)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    base = torch.randn((64, 1), generator=g, device="cuda").bfloat16()
+    fs = [torch.randn((1, 3), generator=g, device="cuda").bfloat16(), torch.randn((1, 2), generator=g, device="cuda").bfloat16()]
+    targets = torch.randint(-1, 6, (64,), generator=g, device="cuda")
+    # (a call of as many tokens as have the same kernel: few tokens add up in another order)
+    want = [v[:64] for v in km.kron_cross_entropy(base.repeat(64, 1), fs, targets.repeat(64))]
+    rows = (1 << 28) + 33
+    got = km.kron_cross_entropy(repeated(base, rows), fs, repeated(targets, rows))
+    assert all(repeats(p, q) for p, q in zip(got, want))
+
+
+def test_gradient_of_a_factor_far_wider_than_its_vocabulary():
+    """2^30 elements and 17 parts of them, all but the vocabulary's zeros."""
+    enough(120)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((17, 16), generator=g, device="cuda").bfloat16()
+    near, second = torch.randn((16, 50), generator=g, device="cuda").bfloat16(), torch.ones((1, 1), device="cuda").bfloat16()
+    targets, dloss = torch.randint(0, 50, (17,), generator=g, device="cuda"), torch.randn(17, generator=g, device="cuda")
+    far = torch.zeros((16, (1 << 26) + 3), dtype=torch.bfloat16, device="cuda")
+    far[:, :50] = near
+    loss, lse = km.kron_cross_entropy(x, (near, second), targets)
+    got = km.kron_cross_entropy(x, (far, second), targets, vocab=50)
+    assert torch.equal(got[0], loss) and torch.equal(got[1], lse)
+    want, (d1, d2) = km.kron_cross_entropy_grad(dloss, x, (near, second), targets, lse)
+    dx, (e1, e2) = km.kron_cross_entropy_grad(dloss, x, (far, second), targets, lse, vocab=50)
+    assert torch.equal(dx, want) and torch.equal(e2, d2) and torch.equal(e1[:, :50], d1)
+    assert not e1[:, 50:].any()
+    del e1, far
+    torch.cuda.empty_cache()
