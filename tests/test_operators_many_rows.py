@@ -74,3 +74,19 @@ def test_gradient_of_a_factor_far_wider_than_its_vocabulary():
     assert not e1[:, 50:].any()
     del e1, far
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("width", [1 << 30, (1 << 30) - 1], ids=["aligned", "odd"])
+def test_statistics_of_the_longest_row(width):
+    """Sums of 2^30 squares: in single precision, a thread's 4 million of them one after the other would lose the small ones (2e-3 of rstd)."""
+    enough(30)
+    x = torch.empty((1, width), dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(5))
+    total = square = 0.0
+    for some in x[0].split(1 << 27):
+        total += float(some.double().sum())
+        square += float(some.double().square().sum())
+    mean = total / width
+    _, got, rstd = km.layer_norm(x, torch.ones(width, dtype=torch.bfloat16, device="cuda"))
+    # sums of blocks, each good to some 2^-24 a step: a thread adds 256 to 2048 elements, then up to 16384 of these sums
+    assert abs(float(got) - mean) <= 1e-5
+    assert abs(float(rstd) * (square / width - mean * mean + 1e-5) ** 0.5 - 1) <= 1e-5
