@@ -402,8 +402,9 @@ km_status kronmatmul_layer_norm_grad(int M, int H, const void* dY, long long ldd
         if (e != hipSuccess) return done(e);
     }
     SumArgs sum = {};
-    sum.job[0] = {(const float*)workspace, dweight, H, 2 * H, parts, H, H};
-    sum.job[1] = {(const float*)workspace + H, dbias, H, 2 * H, parts, H, H};
+    const int64_t apart = 2 * (int64_t)H;
+    sum.job[0] = {(const float*)workspace, dweight, H, apart, parts, H, H};
+    sum.job[1] = {(const float*)workspace + H, dbias, H, apart, parts, H, H};
     return done(sum_up(sum, dbias ? 2 : 1, dtype, (hipStream_t)stream));
 }
 

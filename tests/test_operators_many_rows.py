@@ -90,3 +90,25 @@ def test_statistics_of_the_longest_row(width):
     # sums of blocks, each good to some 2^-24 a step: a thread adds 256 to 2048 elements, then up to 16384 of these sums
     assert abs(float(got) - mean) <= 1e-5
     assert abs(float(rstd) * (square / width - mean * mean + 1e-5) ** 0.5 - 1) <= 1e-5
+
+
+def test_gradients_of_the_longest_row():
+    """2^30 elements, two rows: the sums over them are right to the last column."""
+    enough(60)
+    h = 1 << 30
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x, dy = (torch.empty((2, h), dtype=torch.bfloat16, device="cuda").normal_(generator=g) for _ in range(2))
+    w = torch.ones(h, dtype=torch.bfloat16, device="cuda")
+    _, mean, rstd = km.layer_norm(x, w)
+    assert float(mean.abs().max()) < 1e-3 and float((rstd - 1).abs().max()) < 1e-3
+    _, dw, db = km.layer_norm_grad(dy, x, w, mean, rstd)
+    for first in range(0, h, h // 8):
+        some = slice(first, first + h // 8)
+        assert torch.equal(db[some], (dy[0, some].float() + dy[1, some].float()).bfloat16())
+        xhat = (x[:, some].float() - mean[:, None]) * rstd[:, None]
+        # (one rounding to bf16 of a sum of two products in single precision)
+        terms = dy[:, some].float() * xhat
+        assert bool(((dw[some].float() - terms.sum(0)).abs() <= 2 ** -8 * terms.sum(0).abs() + 2 ** -22 * terms.abs().sum(0)).all())
+        del xhat, terms
+    del x, dy, w, dw, db
+    torch.cuda.empty_cache()
