@@ -1,4 +1,4 @@
-// The backward pass of the gated block and of the loss.  Z_t is computed again block by block (nothing of the size of Z is ever
+// The backward pass of the gated block and of the loss.  Z_t is computed again block by block (it is never
 // written), becomes dZ_t in the registers in which it is, and all four products that follow from it are taken at once:
 //     dU_t = F1 dZ_t,   dX_t = dU_t F2^T,   dF1 = sum_t U_t dZ_t^T,   dF2 = sum_t X_t^T dU_t.
 //
@@ -7,7 +7,8 @@
 // add over q2, so U, dZ (a chunk of C1 rows q1 at a time) and dU go through LDS, and the wavefronts share the results' blocks instead.  Everything is
 // written to LDS as the fragments that lie in registers; where a product needs an operand the other way round (F1 for dU, X for dF2, all
 // of those of dF1 and dX) it is read crossed, so each lies there once.  dF1 and dF2 stay in registers until the tokens are done; the S
-// workgroups' sums are added up in a fixed order by sum_parts.  Where the columns need more than one block, dX is a sum too.
+// workgroups' sums are added up in a fixed order by sum_parts.  Where the columns need more than one block, dX is a sum too, of an fp32 part
+// from each block.
 //
 // bf16: Z from U in two parts, as in the forward pass (the probabilities have to fit the forward pass's sum); dZ, dU and the U of dF1 are rounded to one
 // bf16 each, as they are where layers keep their activations and gradients in bf16.  A gradient so has two such roundings before its own, errors of
@@ -38,6 +39,7 @@ struct GradArgs {
     int tokens, P1, Q1, P2, Q2, ld1, n2;   // as in ForwardArgs
     int q1_step;                           // columns q1 of a block: a multiple of C1, at most R1
     int f_vec, dx_parts;                   // the factors can be read four elements at a time
+    int add;                               // dF1's and dF2's parts are added to what is there, of earlier tokens
 };
 
 // Sizes of a variant: P1 <= 32*KC1, P2 <= 32*KC2; W wavefronts of 16*N columns; R1 and C1 as above; DEEP buffers of a chunk's dZ (with two, a
@@ -503,33 +505,41 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
     }
 
     // this workgroup's sums: dF1 is one of its columns q1 and a part for each (slice of tokens, block of q2); dF2 likewise
+    auto leave = [&](auto more) __attribute__((always_inline)) {
+        auto put = [](float* to, float v) __attribute__((always_inline)) {
+            if constexpr (decltype(more)::value) v += *to;
+            *to = v;
+        };
 #pragma unroll
-    for (int b = 0; b < BR; ++b) {
-        float* const o1 = a.df1[b] + (int64_t)(blockIdx.x * gridDim.z + blockIdx.z) * a.P1 * a.ld1;
+        for (int b = 0; b < BR; ++b) {
+            float* const o1 = a.df1[b] + (int64_t)(blockIdx.x * gridDim.z + blockIdx.z) * a.P1 * a.ld1;
 #pragma unroll
-        for (int ch = 0; ch < CHUNKS; ++ch)
+            for (int ch = 0; ch < CHUNKS; ++ch)
 #pragma unroll
-            for (int d = 0; d < Sh::EP; ++d)
+                for (int d = 0; d < Sh::EP; ++d)
 #pragma unroll
-                for (int e = 0; e < Sh::EQ; ++e) {
-                    const int i = wp + d * Sh::WP, q1 = (ch * BC + wq + e * Sh::WQ) * 16 + c;
+                    for (int e = 0; e < Sh::EQ; ++e) {
+                        const int i = wp + d * Sh::WP, q1 = (ch * BC + wq + e * Sh::WQ) * 16 + c;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int p1 = 16 * i + 4 * g + r;
+                            if (i < B1 && p1 < a.P1 && q1 < q1_count) put(o1 + (int64_t)p1 * a.ld1 + q1_first + q1, df1[ch][b][d][e][r]);
+                        }
+                    }
+            float* const o2 = a.df2[b] + (int64_t)(blockIdx.x * gridDim.y + blockIdx.y) * a.P2 * a.Q2;
+#pragma unroll
+            for (int i = 0; i < B2; ++i)
+#pragma unroll
+                for (int n = 0; n < N; ++n)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const int p1 = 16 * i + 4 * g + r;
-                        if (i < B1 && p1 < a.P1 && q1 < q1_count) o1[(int64_t)p1 * a.ld1 + q1_first + q1] = df1[ch][b][d][e][r];
+                        const int p2 = 16 * i + 4 * g + r;
+                        if (p2 < a.P2 && col + n < q2_count) put(o2 + (int64_t)p2 * a.Q2 + q2_first + col + n, df2[b][i][n][r]);
                     }
-                }
-        float* const o2 = a.df2[b] + (int64_t)(blockIdx.x * gridDim.y + blockIdx.y) * a.P2 * a.Q2;
-#pragma unroll
-        for (int i = 0; i < B2; ++i)
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int p2 = 16 * i + 4 * g + r;
-                    if (p2 < a.P2 && col + n < q2_count) o2[(int64_t)p2 * a.Q2 + q2_first + col + n] = df2[b][i][n][r];
-                }
-    }
+        }
+    };
+    if (a.add) leave(Yes());
+    else leave(No());
 }
 
 }  // namespace km

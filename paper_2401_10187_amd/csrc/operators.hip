@@ -245,9 +245,16 @@ struct GradPlan {
     int q1_step;
     dim3 grid;
     bool dx_parts;
+    int tokens;                            // of a launch
     int parts1, parts2;                    // of dF1 and dF2
     size_t df1, df2, dx, bytes;            // bytes of a branch's parts; of dX's; of everything
 };
+
+// Blocks of columns each leave a part of dX.  Tokens are taken some at a time, so that a launch's parts are no more bytes than these (or one token's for each
+// workgroup): they are summed up right after it, and the next launch has the same place.  Each launch brings the factors into LDS again and has workgroups that
+// wait for the last one.  4096 tokens, bf16 gated 128x128,128x256: 2.1 GB in one launch 3.88 ms, in two 3.96, in nine of 256 MiB 4.39; fp32 loss
+// 128x128,128x256: 4.3 GB 7.91 ms, in five 8.15, in 17 8.42.
+constexpr size_t DX_PARTS = (size_t)1 << 30;
 
 GradPlan plan_grad(int op, km_dtype dtype, int M, const Shape& s, Columns cols)
 {
@@ -273,7 +280,14 @@ GradPlan plan_grad(int op, km_dtype dtype, int M, const Shape& s, Columns cols)
     const int branches = op == OP_LOSS ? 1 : 2;
     p.df1 = piece((size_t)p.parts1 * s.P1 * s.Q1 * 4);
     p.df2 = piece((size_t)p.parts2 * s.P2 * s.Q2 * 4);
-    p.dx = p.dx_parts ? piece((size_t)ny * nz * M * s.P1 * s.P2 * 4) : 0;
+    p.tokens = M;
+    p.dx = 0;
+    if (p.dx_parts && M) {
+        const size_t token = (size_t)ny * nz * s.P1 * s.P2 * 4, most = DX_PARTS / token / slices;
+        const int64_t launch = (most ? most : 1) * slices, launches = (M + launch - 1) / launch, even = up((M + launches - 1) / launches, slices);
+        p.tokens = (int)(even < M ? even : M);
+        p.dx = piece(token * p.tokens);
+    }
     p.bytes = M ? branches * (p.df1 + p.df2) + p.dx : 0;
     return p;
 }
@@ -287,7 +301,7 @@ km_status run_grad(int op, km_dtype dtype, int M, const Shape& s, Columns cols, 
     const km_status ws = check_workspace(p.bytes, workspace, workspace_bytes);
     if (ws != KM_OK) return ws;
     const int branches = op == OP_LOSS ? 1 : 2;
-    const int64_t n1 = (int64_t)s.P1 * s.Q1, n2 = (int64_t)s.P2 * s.Q2, nx = (int64_t)M * s.P1 * s.P2;
+    const int64_t n1 = (int64_t)s.P1 * s.Q1, n2 = (int64_t)s.P2 * s.Q2, row = (int64_t)s.P1 * s.P2, size = (int64_t)element_size(dtype);
     SumArgs sum = {};
     int jobs = 0;
     char* at = (char*)workspace;
@@ -299,20 +313,36 @@ km_status run_grad(int op, km_dtype dtype, int M, const Shape& s, Columns cols, 
         sum.job[jobs++] = {a.df1[b], out[0], n1, n1, M ? p.parts1 : 0, s.Q1, cols.q1};
         sum.job[jobs++] = {a.df2[b], out[1], n2, n2, M ? p.parts2 : 0, s.Q2, cols.q2};
     }
-    if (M) {
-        a.dx = dX;
-        a.dx_parts = p.dx_parts;
-        if (p.dx_parts) {
-            a.dx = at;
-            sum.job[jobs++] = {(const float*)at, dX, nx, nx, (int)(p.grid.y * p.grid.z), nx, nx};
+    a.P1 = s.P1; a.P2 = s.P2; a.Q2 = s.Q2; a.ld1 = s.Q1;
+    a.Q1 = cols.q1; a.n2 = cols.q2;
+    a.q1_step = p.q1_step;
+    a.f_vec = factors_vec(a.f1, a.f2, s, branches, (int)size);
+    a.dx_parts = p.dx_parts;
+    for (int64_t first = 0; first < M; first += p.tokens) {
+        GradArgs some = a;
+        some.tokens = (int)(M - first < p.tokens ? M - first : p.tokens);
+        some.add = first > 0;
+        some.x = (const char*)a.x + first * a.ldx * size;
+        if (a.dh) some.dh = (const char*)a.dh + first * a.lddh * size;
+        if (op == OP_LOSS) {
+            some.targets += first;
+            some.dloss += first;
+            some.lse += first;
         }
-        a.tokens = M;
-        a.P1 = s.P1; a.P2 = s.P2; a.Q2 = s.Q2; a.ld1 = s.Q1;
-        a.Q1 = cols.q1; a.n2 = cols.q2;
-        a.q1_step = p.q1_step;
-        a.f_vec = factors_vec(a.f1, a.f2, s, branches, (int)element_size(dtype));
-        const hipError_t e = p.v->launch(a, p.grid, stream);
+        void* const dx = (char*)dX + first * row * size;
+        some.dx = p.dx_parts ? at : dx;
+        hipError_t e = p.v->launch(some, p.grid, stream);
         if (e != hipSuccess) return done(e);
+        if (!p.dx_parts) continue;
+        const int64_t n = some.tokens * row;
+        const SumJob job = {(const float*)at, dx, n, n, (int)(p.grid.y * p.grid.z), n, n};
+        if (first + p.tokens >= M) sum.job[jobs++] = job;
+        else {
+            SumArgs parts = {};
+            parts.job[0] = job;
+            e = sum_up(parts, 1, dtype, stream);
+            if (e != hipSuccess) return done(e);
+        }
     }
     return done(sum_up(sum, jobs, dtype, stream));
 }
