@@ -8,6 +8,7 @@ Products have two factors, (F1, F2) of P1 x Q1 and P2 x Q2 with P1, P2 up to 128
 Every call is asynchronous on `stream` (a raw hipStream_t value; default: torch's current stream), on which its results and its
 workspace are allocated too.  Inputs made on another stream are the caller's to wait for and to keep, as with any torch operation."""
 import ctypes
+import operator
 from contextlib import nullcontext
 
 from . import binding
@@ -227,7 +228,7 @@ def _loss_arguments(X, Fs, targets, vocab):
     P, Q, pf, shapes = _factors("Fs", Fs, X)
     _vector("targets", targets, X.shape[0], torch.int64, X.get_device())
     columns = shapes[1] * shapes[3]
-    vocab = columns if vocab is None else int(vocab)
+    vocab = columns if vocab is None else operator.index(vocab)
     if not 1 <= vocab <= columns:
         raise ValueError("vocab must be 1 to %d" % columns)
     return code, ldx, P, Q, pf, vocab
