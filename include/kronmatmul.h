@@ -269,9 +269,9 @@ km_status kronmatmul_release(void);
  *   - M up to 2^30.  M == 0 is no error: gradients of weights and factors are then set to zero.
  *   - None of them allocates; the workspace must be 16-byte aligned, may be NULL where the size is 0, need not be
  *     cleared, and is free again when the call's work on the stream is done.
- *   - Workspaces: the loss 8 bytes a token and block of columns; the gradients of factors 4 bytes an element for each workgroup,
- *     of which there are 256 at most or one for each block of columns (32 to 256 of either factor), and, where there are several blocks,
- *     up to 1 GiB of fp32 parts of dX (more tokens take more launches); layer norm's gradient 2 * H floats for each of up to 256 workgroups.
+ *   - Workspaces: the loss 8 bytes a token and block of columns; the gradients of factors 4 bytes an element for each workgroup
+ *     and once more, with 256 workgroups at most or one for each block of columns (32 to 256 of either factor); where there are several
+ *     blocks, up to 1 GiB of fp32 parts of dX besides (more tokens take more launches); layer norm's gradient 2 * H floats for each of up to 256 workgroups.
  *   - Results do not depend on timing: the same call gives the same bits.
  *   - A row of X that holds an infinity or a NaN has results that are no numbers (NaN also where the products' plain sums
  *     would stay infinite), its own only: no other row's results change.  The factors' and weights' gradients are sums over

@@ -39,7 +39,6 @@ struct GradArgs {
     int tokens, P1, Q1, P2, Q2, ld1, n2;   // as in ForwardArgs
     int q1_step;                           // columns q1 of a block: a multiple of C1, at most R1
     int f_vec, dx_parts;                   // the factors can be read four elements at a time
-    int add;                               // dF1's and dF2's parts are added to what is there, of earlier tokens
 };
 
 // Sizes of a variant: P1 <= 32*KC1, P2 <= 32*KC2; W wavefronts of 16*N columns; R1 and C1 as above; DEEP buffers of a chunk's dZ (with two, a
@@ -109,6 +108,9 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
     // Sums over q2 leave out what is past its end.  (A gated block in fp32, 1000 tokens 52x50,65x20: 107 -> 92 us; with all columns full the branch costs 2%.  The
     // loss's columns are many; bf16's products are short.)
     constexpr bool FEW_COLUMNS = !SPLIT && OP != OP_LOSS;
+    // (The gated kernels ask whether a row is short in classes without short ones too: 2000 tokens 52x50,65x20 bf16 143 us, 172 without the question,
+    // 64x128,64x128 130 and 126; the loss, 8192 tokens 64x256,64x256: 574 us with it, 534 without.)
+    constexpr bool WHOLE = OP == OP_LOSS && KC1 * KC2 > 1;
     extern __shared__ __align__(32) unsigned char smem[];
     T* const s1 = reinterpret_cast<T*>(smem);
     T* const sz = s1 + BR * Sh::F1;                        // (what chunks read is within the 64 KB that one address register reaches)
@@ -160,14 +162,14 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
 #pragma unroll
         for (int i = 0; i < Sh::XAHEAD; ++i) {
             const int piece = tid + i * THREADS, p1 = piece * magic >> 16, k = 8 * (piece - p1 * row_pieces);
-            xp[i] = eight_of_row<(KC1 * KC2 > 1)>(x, p1 * a.P2 + k, piece < pieces, total, a.P2 % 8 != 0, i == 0);
+            xp[i] = eight_of_row<WHOLE>(x, p1 * a.P2 + k, piece < pieces, total, a.P2 % 8 != 0, i == 0);
         }
     };
     auto store_x = [&](const T* x) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < Sh::XPIECES; ++i) {
             const int piece = tid + i * THREADS, p1 = piece * magic >> 16, k = 8 * (piece - p1 * row_pieces);
-            if (piece < pieces) at.put_straight(sx, mixed_row(p1), k, KC2, i < Sh::XAHEAD ? xp[i] : eight_of_row<(KC1 * KC2 > 1)>(x, p1 * a.P2 + k, true, total, a.P2 % 8 != 0, false));
+            if (piece < pieces) at.put_straight(sx, mixed_row(p1), k, KC2, i < Sh::XAHEAD ? xp[i] : eight_of_row<WHOLE>(x, p1 * a.P2 + k, true, total, a.P2 % 8 != 0, false));
         }
     };
 
@@ -272,7 +274,7 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
 #pragma unroll
                 for (int i = 0; i < B1; ++i) {
                     const Frag xf = Sh::XLDS ? at.get(sx, i * KC2 + k)
-                                             : eight_of_row<(KC1 * KC2 > 1)>(x, mixed_row(16 * i + c) * a.P2 + 32 * k + 8 * g, mixed_row(16 * i + c) < a.P1 && 32 * k + 8 * g < a.P2, total, a.P2 % 8 != 0, true);
+                                             : eight_of_row<WHOLE>(x, mixed_row(16 * i + c) * a.P2 + 32 * k + 8 * g, mixed_row(16 * i + c) < a.P1 && 32 * k + 8 * g < a.P2, total, a.P2 % 8 != 0, true);
 #pragma unroll
                     for (int n = 0; n < N; ++n) Op<T>::mma(du[b][i][n], xf, f[n]);
                 }
@@ -505,41 +507,33 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
     }
 
     // this workgroup's sums: dF1 is one of its columns q1 and a part for each (slice of tokens, block of q2); dF2 likewise
-    auto leave = [&](auto more) __attribute__((always_inline)) {
-        auto put = [](float* to, float v) __attribute__((always_inline)) {
-            if constexpr (decltype(more)::value) v += *to;
-            *to = v;
-        };
 #pragma unroll
-        for (int b = 0; b < BR; ++b) {
-            float* const o1 = a.df1[b] + (int64_t)(blockIdx.x * gridDim.z + blockIdx.z) * a.P1 * a.ld1;
+    for (int b = 0; b < BR; ++b) {
+        float* const o1 = a.df1[b] + (int64_t)(blockIdx.x * gridDim.z + blockIdx.z) * a.P1 * a.ld1;
 #pragma unroll
-            for (int ch = 0; ch < CHUNKS; ++ch)
+        for (int ch = 0; ch < CHUNKS; ++ch)
 #pragma unroll
-                for (int d = 0; d < Sh::EP; ++d)
+            for (int d = 0; d < Sh::EP; ++d)
 #pragma unroll
-                    for (int e = 0; e < Sh::EQ; ++e) {
-                        const int i = wp + d * Sh::WP, q1 = (ch * BC + wq + e * Sh::WQ) * 16 + c;
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int p1 = 16 * i + 4 * g + r;
-                            if (i < B1 && p1 < a.P1 && q1 < q1_count) put(o1 + (int64_t)p1 * a.ld1 + q1_first + q1, df1[ch][b][d][e][r]);
-                        }
-                    }
-            float* const o2 = a.df2[b] + (int64_t)(blockIdx.x * gridDim.y + blockIdx.y) * a.P2 * a.Q2;
-#pragma unroll
-            for (int i = 0; i < B2; ++i)
-#pragma unroll
-                for (int n = 0; n < N; ++n)
+                for (int e = 0; e < Sh::EQ; ++e) {
+                    const int i = wp + d * Sh::WP, q1 = (ch * BC + wq + e * Sh::WQ) * 16 + c;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const int p2 = 16 * i + 4 * g + r;
-                        if (p2 < a.P2 && col + n < q2_count) put(o2 + (int64_t)p2 * a.Q2 + q2_first + col + n, df2[b][i][n][r]);
+                        const int p1 = 16 * i + 4 * g + r;
+                        if (i < B1 && p1 < a.P1 && q1 < q1_count) o1[(int64_t)p1 * a.ld1 + q1_first + q1] = df1[ch][b][d][e][r];
                     }
-        }
-    };
-    if (a.add) leave(Yes());
-    else leave(No());
+                }
+        float* const o2 = a.df2[b] + (int64_t)(blockIdx.x * gridDim.y + blockIdx.y) * a.P2 * a.Q2;
+#pragma unroll
+        for (int i = 0; i < B2; ++i)
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int p2 = 16 * i + 4 * g + r;
+                    if (p2 < a.P2 && col + n < q2_count) o2[(int64_t)p2 * a.Q2 + q2_first + col + n] = df2[b][i][n][r];
+                }
+    }
 }
 
 }  // namespace km

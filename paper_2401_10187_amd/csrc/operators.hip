@@ -247,13 +247,13 @@ struct GradPlan {
     bool dx_parts;
     int tokens;                            // of a launch
     int parts1, parts2;                    // of dF1 and dF2
-    size_t df1, df2, dx, bytes;            // bytes of a branch's parts; of dX's; of everything
+    size_t df1, df2, dx, bytes;            // bytes of a branch's parts, with several launches of their sum in front of them; of dX's; of everything
 };
 
 // Blocks of columns each leave a part of dX.  Tokens are taken some at a time, so that a launch's parts are no more bytes than these (or one token's for each
-// workgroup): they are summed up right after it, and the next launch has the same place.  Each launch brings the factors into LDS again and has workgroups that
-// wait for the last one.  4096 tokens, bf16 gated 128x128,128x256: 2.1 GB in one launch 3.88 ms, in two 3.96, in nine of 256 MiB 4.39; fp32 loss
-// 128x128,128x256: 4.3 GB 7.91 ms, in five 8.15, in 17 8.42.
+// workgroup): they are summed up right after it, and the next launch has the same place.  So are the factors' parts, together with the sums so far.
+// Each launch brings the factors into LDS again and has workgroups that wait for the last one.  4096 tokens, bf16 gated 128x128,128x256: 2.1 GB in one launch
+// 4.08 ms, in two 4.12, in nine of 256 MiB 4.33; fp32 loss 128x128,128x256: 4.3 GB in one 7.62, in five 7.82, in 17 7.90.
 constexpr size_t DX_PARTS = (size_t)1 << 30;
 
 GradPlan plan_grad(int op, km_dtype dtype, int M, const Shape& s, Columns cols)
@@ -278,8 +278,6 @@ GradPlan plan_grad(int op, km_dtype dtype, int M, const Shape& s, Columns cols)
     p.parts1 = slices * nz;
     p.parts2 = slices * ny;
     const int branches = op == OP_LOSS ? 1 : 2;
-    p.df1 = piece((size_t)p.parts1 * s.P1 * s.Q1 * 4);
-    p.df2 = piece((size_t)p.parts2 * s.P2 * s.Q2 * 4);
     p.tokens = M;
     p.dx = 0;
     if (p.dx_parts && M) {
@@ -288,6 +286,9 @@ GradPlan plan_grad(int op, km_dtype dtype, int M, const Shape& s, Columns cols)
         p.tokens = (int)(even < M ? even : M);
         p.dx = piece(token * p.tokens);
     }
+    const int sums = p.tokens < M;
+    p.df1 = piece((size_t)(p.parts1 + sums) * s.P1 * s.Q1 * 4);
+    p.df2 = piece((size_t)(p.parts2 + sums) * s.P2 * s.Q2 * 4);
     p.bytes = M ? branches * (p.df1 + p.df2) + p.dx : 0;
     return p;
 }
@@ -302,16 +303,20 @@ km_status run_grad(int op, km_dtype dtype, int M, const Shape& s, Columns cols, 
     if (ws != KM_OK) return ws;
     const int branches = op == OP_LOSS ? 1 : 2;
     const int64_t n1 = (int64_t)s.P1 * s.Q1, n2 = (int64_t)s.P2 * s.Q2, row = (int64_t)s.P1 * s.P2, size = (int64_t)element_size(dtype);
-    SumArgs sum = {};
+    const bool several = p.tokens < M;     // launches: sums of those before are one part more, in front of the others
+    SumArgs sum = {}, far = {};            // the last launch's sums; those before
     int jobs = 0;
     char* at = (char*)workspace;
     for (int b = 0; b < branches; ++b) {
         void* const* out = b ? d2 : d1;
-        a.df1[b] = (float*)at;
-        a.df2[b] = (float*)(at + p.df1);
+        float *const s1 = (float*)at, *const s2 = (float*)(at + p.df1);
+        a.df1[b] = several ? s1 + n1 : s1;
+        a.df2[b] = several ? s2 + n2 : s2;
         at += p.df1 + p.df2;
-        sum.job[jobs++] = {a.df1[b], out[0], n1, n1, M ? p.parts1 : 0, s.Q1, cols.q1};
-        sum.job[jobs++] = {a.df2[b], out[1], n2, n2, M ? p.parts2 : 0, s.Q2, cols.q2};
+        far.job[jobs] = {a.df1[b], s1, n1, n1, p.parts1, s.Q1, cols.q1};
+        far.job[jobs + 1] = {a.df2[b], s2, n2, n2, p.parts2, s.Q2, cols.q2};
+        sum.job[jobs++] = {s1, out[0], n1, n1, M ? p.parts1 + several : 0, s.Q1, cols.q1};
+        sum.job[jobs++] = {s2, out[1], n2, n2, M ? p.parts2 + several : 0, s.Q2, cols.q2};
     }
     a.P1 = s.P1; a.P2 = s.P2; a.Q2 = s.Q2; a.ld1 = s.Q1;
     a.Q1 = cols.q1; a.n2 = cols.q2;
@@ -321,7 +326,6 @@ km_status run_grad(int op, km_dtype dtype, int M, const Shape& s, Columns cols, 
     for (int64_t first = 0; first < M; first += p.tokens) {
         GradArgs some = a;
         some.tokens = (int)(M - first < p.tokens ? M - first : p.tokens);
-        some.add = first > 0;
         some.x = (const char*)a.x + first * a.ldx * size;
         if (a.dh) some.dh = (const char*)a.dh + first * a.lddh * size;
         if (op == OP_LOSS) {
@@ -336,12 +340,18 @@ km_status run_grad(int op, km_dtype dtype, int M, const Shape& s, Columns cols, 
         if (!p.dx_parts) continue;
         const int64_t n = some.tokens * row;
         const SumJob job = {(const float*)at, dx, n, n, (int)(p.grid.y * p.grid.z), n, n};
-        if (first + p.tokens >= M) sum.job[jobs++] = job;
-        else {
-            SumArgs parts = {};
-            parts.job[0] = job;
-            e = sum_up(parts, 1, dtype, stream);
-            if (e != hipSuccess) return done(e);
+        if (first + p.tokens >= M) {
+            sum.job[jobs++] = job;
+            break;
+        }
+        SumArgs parts = {};
+        parts.job[0] = job;
+        e = sum_up(parts, 1, dtype, stream);
+        if (e == hipSuccess) e = sum_up(far, jobs, KM_F32, stream);
+        if (e != hipSuccess) return done(e);
+        for (int i = 0; first == 0 && i < jobs; ++i) {
+            far.job[i].in = sum.job[i].in;
+            far.job[i].parts = sum.job[i].parts;
         }
     }
     return done(sum_up(sum, jobs, dtype, stream));
