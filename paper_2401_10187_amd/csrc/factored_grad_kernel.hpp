@@ -187,7 +187,7 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
     };
     // Logits that are no word's: in columns past n2, in rows past Q1, and in the last column q1 of a vocabulary in some columns q2.  Wavefronts and
     // chunks that hold some mask them, in the form that also takes the 1 off the target.  (F1's zeros there do not: Z is -lse, whose exponential may be infinite.)
-    const bool edge = OP == OP_LOSS && (wave + 1) * 16 * N > q2_count;
+    const bool edge = OP == OP_LOSS && (wave + 1) * 16 * N > q2_count, idle = OP == OP_LOSS && wave * 16 * N >= q2_count;
     int words[N];                          // columns q1 of the block, from the first, that are words in each of this lane's columns q2
 #pragma unroll
     for (int n = 0; n < N; ++n) words[n] = col + n < q2_count ? a.Q1 - q1_first - (OP == OP_LOSS && (int64_t)(a.Q1 - 1) * a.Q2 + q2_first + col + n >= a.vocab) : 0;
@@ -419,6 +419,7 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
         };
         auto z_of = [&](int ch) __attribute__((always_inline)) {
             if constexpr (OP == OP_LOSS) {
+                if (idle) return;          // (its part of dZ stays zeros)
                 if (edge || ch == cut_chunk || ch == target_chunk) z_part(ch, Yes());
                 else z_part(ch, No());
             } else z_part(ch, No());
