@@ -232,7 +232,7 @@ ForwardPlan plan_forward(int op, km_dtype dtype, int M, const Shape& s, Columns 
     auto nz = [&] { return (cols.q2 + p.q2_step - 1) / p.q2_step; };
     while ((int64_t)M * ny() * nz() < UNITS && p.q2_step > unit) p.q2_step = halve(p.q2_step, unit);
     const int64_t own = (int64_t)M * (p.q2_step / unit);                       // units of a block of columns
-    p.threads = own * 64 >= p.v->threads ? p.v->threads : own >= 8 ? 512 : 256;
+    p.threads = own * 64 >= p.v->threads ? p.v->threads : 256;
     const int64_t groups = (own + p.threads / 64 - 1) / (p.threads / 64), some = up(UNITS, (int64_t)ny() * nz()) / ((int64_t)ny() * nz());
     p.grid = dim3((unsigned)(groups < some ? groups : some), ny(), nz());
     p.lds = (int)(column1 * p.q1_step + column2 * p.q2_step);
