@@ -321,7 +321,7 @@ template <bool WHOLE, typename T> __device__ __forceinline__ typename Op<T>::Fra
 
 // The activation of a gate and its derivative.  Both activations are z * sigma(v), sigma the logistic function: v = z (SiLU), or
 // v = 2c(z + 0.044715 z^3) with c = sqrt(2/pi), which is GELU's form with tanh, since (1 + tanh w)/2 = sigma(2w).  So
-// neither end cancels: exp(-v) overflows to infinity where 1/(1+inf) = 0 is right.  dv stays a number for any z, so that sigma's slope of 0 takes it away.
+// neither end cancels, and v_rcp's last place is enough: exp(-v) overflows to infinity where 1/(1+inf) = 0 is right.  dv stays a number for any z, so that sigma's slope of 0 takes it away.
 template <bool GELU> __device__ __forceinline__ float activate(float z, float& slope)
 {
     const float c2 = 1.5957691216057308f;

@@ -9,10 +9,10 @@
 //
 // Bounds and figures, bf16, 8192 tokens:
 //   gated 64x128,64x128  112 us: 86 GFLOP (both parts of U counted; 770 TFLOP/s), 336 MB (3.0 TB/s).  A result costs 11 vector instructions, two
-//       of them at a quarter of the rate, so that the vector units are busy for 65% of the time and the matrix cores for 40%, and the two wavefronts of a
+//       of them at a quarter of the rate, so that the vector units are busy for 62% of the time and the matrix cores for 39%, and the two wavefronts of a
 //       SIMD hide only part of one behind the other.  Units of 32 columns, four wavefronts a SIMD, the next block's products among a block's
 //       activations, X a unit ahead: 121, 148, 134, 117 us.
-//   loss 64x256,64x256  152 us: 155 GFLOP (1020 TFLOP/s) and 537 million exponentials and additions: vector units 69%, matrix cores 45%.
+//   loss 64x256,64x256  147 us with loss_join: 155 GFLOP (1050 TFLOP/s) and 537 million exponentials and additions: vector units 69%, matrix cores 46%.
 #pragma once
 #include "factored_core.hpp"
 

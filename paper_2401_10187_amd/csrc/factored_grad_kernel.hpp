@@ -12,10 +12,11 @@
 //
 // bf16: Z from U in two parts, as in the forward pass (the probabilities have to fit the forward pass's sum); dZ, dU and the U of dF1 are rounded to one
 // bf16 each, as they are where layers keep their activations and gradients in bf16.  A gradient so has two such roundings before its own, errors of
-// 2.9e-3 of its norm where one rounding leaves 1.7e-3.  With dU in two parts dX and dF2 would have 2.4e-3, and the gated kernel take 357 us instead of
-// 308 (8192 tokens 64x128,64x128); with dZ in two parts for dU 387, for dF1 too 662.
+// 2.9e-3 of its norm where one rounding leaves 1.7e-3 (2.3e-3 for the loss: where p is small the target's dZ is near -1, which bf16 holds).  The target's dZ is
+// p - 1 before it is rounded, so that likely targets have no larger errors.  With dU in two parts dX and dF2 would have 2.4e-3, and the gated kernel
+// take 357 us instead of 308 (8192 tokens 64x128,64x128); with dZ in two parts for dU 387, for dF1 too 662.
 //
-// Bounds and figures, bf16, 8192 tokens: gated 64x128,64x128 308 us, 189 GFLOP with both parts of U (610 TFLOP/s); loss 64x256,64x256 395 us, 326 GFLOP (825
+// Bounds and figures, bf16, 8192 tokens: gated 64x128,64x128 308 us, 189 GFLOP with both parts of U (610 TFLOP/s); loss 64x256,64x256 390 us, 326 GFLOP (835
 // TFLOP/s).  Matrix cores, vector units and LDS are each busy for 30 to 50% of the time; the rest are waits that the two wavefronts of a SIMD, held
 // together by a barrier for each chunk, do not hide from each other.  About 30 us of it are the factors on their way into LDS and the sums on
 // their way out.  More wavefronts have no registers; four of 32 columns, two tokens in turn, waves half a chunk apart: no quicker.
@@ -105,8 +106,9 @@ __global__ __launch_bounds__(Sh::W * 64) void factored_grad(GradArgs a)
     constexpr int OP = Sh::OP, BR = Sh::BR, KC1 = Sh::KC1, KC2 = Sh::KC2, N = Sh::N, W = Sh::W, KCQ = Sh::KCQ, B1 = Sh::B1, B2 = Sh::B2, BC = Sh::BC;
     constexpr int CHUNKS = Sh::R1 / Sh::C1, THREADS = W * 64;
     constexpr bool SPLIT = Op<T>::split;
-    // Sums over q2 leave out what is past its end.  (A gated block in fp32, 1000 tokens 52x50,65x20: 107 -> 92 us; with all columns full the branch costs 2%.  The
-    // loss's columns are many; bf16's products are short.)
+    // Sums over q2 leave out what is past its end.  (Forward and backward, with and without: the gated block in fp32, 1000 tokens 52x50,65x20 111 and 127 us, 64x64,64x64
+    // 120 and 118, 32x64,32x100 106 and 104.  bf16's products are short, and the branch keeps them apart: 2000 tokens 64x128,64x128 131 and 126 us, though 52x50,65x20
+    // 115 and 142.  The loss's columns are many: 1000 tokens 64x256,64x256 bf16 101 and 96, 32x128,64x256 fp32 156 and 152, though 32x128,64x33 77 and 82.)
     constexpr bool FEW_COLUMNS = !SPLIT && OP != OP_LOSS;
     // (The gated kernels ask whether a row is short in classes without short ones too: 2000 tokens 52x50,65x20 bf16 143 us, 172 without the question,
     // 64x128,64x128 130 and 126; the loss, 8192 tokens 64x256,64x256: 574 us with it, 534 without.)

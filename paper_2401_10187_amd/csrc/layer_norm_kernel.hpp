@@ -4,8 +4,8 @@
 // thread, and keeps it in registers between the row's mean, the sum of squares about that mean (which so cannot cancel) and the
 // results.  The backward pass needs two sums of a row, sum dxhat and sum dxhat xhat; each thread also adds up dw and db of the columns that are
 // its own in every row, in fp32.  A workgroup's teams join theirs in LDS, in their order, and the workgroups' sums are added
-// by sum_parts, so the result does not depend on timing.  Bound by memory; few rows: by latency.  8192 rows of 4096 bf16: forward 25 us
-// (5.4 TB/s, part of it from the last-level cache), backward 44 us (4.6 TB/s) and 5 us of sum_parts; one row: 3 us.
+// by sum_parts, so the result does not depend on timing.  Bound by memory; few rows: by latency.  8192 rows of 4096 bf16: forward 25.8 us
+// (5.2 TB/s, part of it from the last-level cache), backward 44.3 us (4.5 TB/s) and 4.7 us of sum_parts; one row: 3.2 us.
 // Rows longer than a team holds are read again for each step (CH = 0).
 #pragma once
 #include "factored_core.hpp"

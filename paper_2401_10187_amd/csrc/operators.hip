@@ -223,8 +223,9 @@ ForwardPlan plan_forward(int op, km_dtype dtype, int M, const Shape& s, Columns 
         else p.q2_step = halve(p.q2_step, unit);
     }
     // few tokens: the columns q1 over more workgroups, until there are four wavefronts with work on each compute unit, or eight if U, which each workgroup
-    // computes again, is no more work than Z (512 tokens 64x128,64x128: fp32 54 us, 73 with four, bf16 16, 18 with four; fp32, 1000 tokens 52x50,65x20, where
-    // it is more: 36 us, 26 with four); four for the loss in bf16, which writes nothing (1294 tokens 105x93,74x4: 24 us, 20 with four)
+    // computes again, is no more work than Z (512 tokens 64x128,64x128: fp32 51 us, 71 with four, bf16 15, 18 with four; 64 tokens of the loss 64x256,64x256 fp32
+    // 16, 21 with four; but 200 tokens 128x128,128x256 fp32 81, 59 with four); four for the loss in bf16, which writes nothing (200 tokens 128x128,128x256 20 us, 26 with
+    // eight; 1294 tokens 105x93,74x4 22 and 25, 32x512,32x64 17 and 19; but 512 tokens 128x512,32x32 18 and 13)
     const int64_t units = (int64_t)M * ((cols.q2 + unit - 1) / unit);
     auto wanted = [&] { return ((op != OP_LOSS || dtype == KM_F32) && 2 * class_of(s.P2) <= p.q1_step / 16 ? 8 : 4) * UNITS; };
     while (p.q1_step > 16 && units * ((cols.q1 + p.q1_step - 1) / p.q1_step) < wanted()) p.q1_step = halve(p.q1_step, 16);
